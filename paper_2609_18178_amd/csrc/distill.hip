@@ -190,7 +190,7 @@ __global__ __launch_bounds__(Threads, Held <= 4 ? 8 : 4) void distill_kernel(con
         uint32_t value;
     };
     struct Listed {
-        float x;       // over T; -infinity: nothing
+        float x;       // the teacher's; -infinity: nothing
         T logit;       // the student's
         int32_t place;
         bool outside;  // of the vocabulary
@@ -214,7 +214,7 @@ __global__ __launch_bounds__(Threads, Held <= 4 ? 8 : 4) void distill_kernel(con
         l.place = some && !l.outside ? (int32_t)i : -1;
         l.logit = T(0);
         if (l.place >= 0) l.logit = row.first[l.place];
-        l.x = some ? x / d.temperature : -kInf;
+        l.x = some ? x : -kInf;
         return l;
     };
     // (Loads are under way in the order of their use: the teacher's slots, the row, the student's logits in them.)
@@ -242,7 +242,8 @@ __global__ __launch_bounds__(Threads, Held <= 4 ? 8 : 4) void distill_kernel(con
     }
     const T beside = row.load_beside(t);
 
-    // the teacher's softmax over its listed slots
+    // the teacher's softmax over its listed slots: as the student's, the difference first, so that logits near the
+    // type's largest or lowest number stay finite at any temperature
     if (t == 0) twice = 0;
     // (NaN counts as the largest: the row is NaN)
     auto size = [](float x) { return x == x ? x : kInf; };
@@ -252,12 +253,13 @@ __global__ __launch_bounds__(Threads, Held <= 4 ? 8 : 4) void distill_kernel(con
             if (lane < d.top) first = listed(first_slot);
             const float x = first.x;
             const float most = over_wave(size(x), Max());
-            const float e = x == -kInf ? 0.0f : __expf(x - most);
+            const float over = (x - most) / d.temperature;
+            const float e = x == -kInf ? 0.0f : __expf(over);
             float total = over_wave(e, Sum());
             if (__builtin_amdgcn_ballot_w64(first.outside) != 0) total = kNan;
             if (lane < d.top) {
                 prob[lane] = x == -kInf ? 0.0f : e / total;
-                excess[lane] = x - most;
+                excess[lane] = over;
                 place[lane] = first.place;
             }
             if (lane == 0) total_of_teacher = total;
@@ -276,9 +278,9 @@ __global__ __launch_bounds__(Threads, Held <= 4 ? 8 : 4) void distill_kernel(con
         most = over_block<Threads>(most, Max(), scratch);
         float total = 0.0f;
         for (uint32_t j = t; j < d.top; j += Threads) {
-            const float x = excess[j], e = x == -kInf ? 0.0f : __expf(x - most);
+            const float x = excess[j], over = (x - most) / d.temperature, e = x == -kInf ? 0.0f : __expf(over);
             prob[j] = e;
-            excess[j] = x - most;
+            excess[j] = over;
             total += e;
         }
         total = over_block<Threads>(total, Sum(), scratch);
