@@ -24,7 +24,8 @@ constexpr uint64_t kMaxItems = UINT32_MAX;
 constexpr uint64_t kCus = 256;
 // A row of FP8 bytes: 256 of them are counted in 32 bits.
 constexpr uint64_t kMaxFp8Row = 1ull << 24;
-// LDS of a workgroup of a product that quantises its rows on the way: two fit a CU.
+// A product of up to so many rows can quantise them on the way, with this LDS a workgroup: two fit a CU.
+constexpr uint64_t kFewRows = 16;
 constexpr uint64_t kFewLds = 64 * 1024;
 constexpr double kLog2e = 1.4426950408889634074;
 
@@ -166,6 +167,10 @@ Parts parts_of(uint64_t m, uint64_t n, uint64_t k) {
 // 2048 11.1 / 9.4, 4096 18.0 / 15.1, 5000 21.3 / 17.4, 14336 37.8 / 40.5; 500 x 3000 x 8192 25.0 / 24.6; 1024 x 2048 x 4096 17.2 / 14.4,
 // 300 x 4096 x 4096 17.7 / 14.7.  From 64 blocks on the parts are left.  Outside of those sizes: 256 x 4096 x 4096 in squares of 64 /
 // halves 12.8 / 14.0; 600 x 4096 x 2048, of 320 halves, in squares of 128 / halves 12.1 / 16.6.
+// Up to 16 rows of a are in squares of 16 however many there are: their waves add in the order of the product that quantises
+// its rows on the way, so that both give the same bits, and the larger squares would be empty in most of their rows.  us, weights out of
+// memory, in the larger squares / of 16, with bf16 and with binary32 result: 1 x 17000 x 4096 23.3 / 16.4, 30.9 / 16.3; 1 x 140000 x 4096 148 / 93,
+// 165 / 94; 16 x 140000 x 4096 154 / 114, 171 / 121; 1 x 140000 x 520 30.1 / 28.3, 36.3 / 33.2; 1 x 65536 x 520 13.3 / 14.9, 16.2 / 17.6.
 // us per product of inputs out of memory, in squares of 16 / 32 / 64 / 128, deep / 128 / 256:
 //                 K = 1024                                  K = 4096
 //     16 x  4096   4.2   5.7   9.7    -  16.9  41     (K = 4096, inputs in cache)
@@ -191,7 +196,7 @@ Cut cut(uint64_t m, uint64_t n, uint64_t k, bool wide) {
     const bool halves = !wide && tiles(64) > kCus && ceil_div(m, 128) * ceil_div(n, 64) <= kCus;
     if (halves && (parts.count <= 1 || k <= 63 * pact::kBlockK)) return {Tile::Narrow128, 128, 256, 0, 64};
     if (parts.count > 1) return {Tile::Deep128, 128, 256, parts.blocks};
-    if (tiles(16) <= 2 * kCus) return {Tile::Shared16, 16, 512};
+    if ((m <= kFewRows && tiles(16) <= kMaxItems / 512) || tiles(16) <= 2 * kCus) return {Tile::Shared16, 16, 512};
     if (tiles(32) <= 2 * kCus) return {Tile::Shared32, 32, 512};
     if (wide && tiles(64) <= kCus && k >= 1024) return {Tile::Shared64Long, 64, 512};
     if (tiles(64) <= (wide ? 2 : 1) * kCus) return {Tile::Shared64, 64, 256};
@@ -249,10 +254,9 @@ uint64_t held_bytes(uint64_t m, uint64_t k) { return round_up(m * round_up(k, PA
 uint64_t held_scale_bytes(uint64_t m, uint64_t k) {
     return round_up(m * round_up(ceil_div(k, PACT_FP8_BLOCK), pact::kScaleGroup), 256);
 }
-// Whether a product of x (m x k) quantises it on its way, in every workgroup.
-constexpr uint64_t kFewRows = 16;
-bool on_the_way(uint64_t m, uint64_t k) {
-    return m <= kFewRows && k < kMaxFp8Row && pact::few_rows_bytes((uint32_t)m, (uint32_t)ceil_div(k, pact::kBlockK)) <= kFewLds;
+// Whether a product of x (m x k) with n rows quantises it on its way, in every workgroup: where it would be in squares of 16.
+bool on_the_way(uint64_t m, uint64_t n, uint64_t k) {
+    return m <= kFewRows && ceil_div(n, 16) <= kMaxItems / 512 && k < kMaxFp8Row && pact::few_rows_bytes((uint32_t)m, (uint32_t)ceil_div(k, pact::kBlockK)) <= kFewLds;
 }
 
 // C = a b^T in one launch (and the joining of the parts of K); with x, of x on the way and no more of `a` than its size.
@@ -472,7 +476,7 @@ int pact_fp8_matmul(const pact_fp8* a, const pact_fp8* b, const pact_matrix* c, 
 
 int64_t pact_fp8_linear_workspace_bytes(uint64_t m, uint64_t n, uint64_t k) {
     if (m >= kMaxRows || n >= kMaxRows || k >= kMaxFp8Row) return PACT_ERANGE;
-    return on_the_way(m, k) ? 0 : (int64_t)(held_at(nullptr, m, k).bytes + sums_bytes(m, n, k));
+    return on_the_way(m, n, k) ? 0 : (int64_t)(held_at(nullptr, m, k).bytes + sums_bytes(m, n, k));
 }
 
 int pact_fp8_linear(const pact_matrix* x, const pact_fp8* w, const pact_matrix* y, void* workspace,
@@ -486,7 +490,7 @@ int pact_fp8_linear(const pact_matrix* x, const pact_fp8* w, const pact_matrix* 
     if ((rc = check_workspace(spans, workspace, workspace_bytes)) != PACT_OK) return rc;
     if (spans.overlap()) return PACT_EOVERLAP;
     const uint64_t m = x->rows, k = x->cols;
-    if (on_the_way(m, k)) {
+    if (on_the_way(m, y->cols, k)) {
         const pact_fp8 size = {nullptr, nullptr, m, k, 0, 0};
         return product(size, *w, *y, false, x, nullptr, static_cast<hipStream_t>(stream));
     }

@@ -1,0 +1,59 @@
+"""What the training operators promise beside their numbers: which calls give the same bits."""
+import pytest
+import torch
+
+import paper_2609_18178_amd as pk
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def _weight(n, k, seed=9):
+    return pk.fp8_quantize((torch.randn(n, k, generator=_gen(seed)) * 0.02).to(DEV), square=True)
+
+
+# rows quantised on the way and in the workspace; squares of every size, halves, parts of K, cut along a side
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 17000, 520), (1, 33000, 4096), (5, 16400, 129), (16, 17000, 520),
+                                   (16, 70001, 1000), (9, 40, 4096), (16, 17000, 4096), (17, 17000, 520), (33, 48, 640),
+                                   (300, 1100, 9000), (513, 2999, 640), (517, 520, 1003), (1100, 260, 385),
+                                   (4201, 4099, 4100)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_linear_is_quantize_and_product_bit_for_bit(m, n, k, dtype):
+    print("linear", m, n, k, dtype, flush=True)
+    w = _weight(n, k)
+    x = torch.randn(m, k, generator=_gen(m)).to(dtype).to(DEV)
+    for out in (torch.float32, torch.bfloat16):
+        assert torch.equal(pk.fp8_linear(x, w, dtype=out), pk.fp8_matmul(pk.fp8_quantize(x), w, dtype=out)), out
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 300, 129), (12, 700, 20000), (300, 9000, 1100), (1100, 600, 513)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_backward_is_quantize_and_products_bit_for_bit(m, n, k, dtype):
+    print("backward", m, n, k, dtype, flush=True)
+    wt = pk.fp8_quantize((torch.randn(n, k, generator=_gen(2)) * 0.05).to(DEV), "columns", square=True)
+    xt = pk.fp8_quantize(torch.randn(m, k, generator=_gen(1)).to(DEV), "columns")
+    dy = (torch.randn(m, n, generator=_gen(3)) * 1e-3).to(dtype).to(DEV)
+    dx, dw = pk.fp8_linear_backward(dy, wt, xt)
+    along_rows, along_columns = pk.fp8_quantize(dy, "both")
+    assert torch.equal(dx, pk.fp8_matmul(along_rows, wt, dtype=dtype))
+    assert torch.equal(dw, pk.fp8_matmul(along_columns, xt, dtype=torch.float32))
+
+
+def test_more_columns_than_squares_of_16_in_a_launch():
+    """A launch has at most 2^32 work-items: beyond 134 million columns few rows are in larger squares, either way."""
+    print("columns", flush=True)
+    n, k = (1 << 27) + 130, 100
+    assert pk._lib().pact_fp8_linear_workspace_bytes(1, (1 << 27) - 16, k) == 0 < pk._lib().pact_fp8_linear_workspace_bytes(1, n, k)
+    part = _weight(300, k)
+    data = torch.zeros(n, 128, dtype=torch.uint8, device=DEV)
+    scale = torch.zeros(n, 4, dtype=torch.uint8, device=DEV)
+    data[-300:], scale[-300:] = part.data, part.scale
+    w = pk.Fp8Matrix(data, scale, k)
+    x = torch.randn(1, k, generator=_gen(4)).to(DEV)
+    got = pk.fp8_linear(x, w)
+    assert torch.equal(got, pk.fp8_matmul(pk.fp8_quantize(x), w))
+    assert not got[:, :-300].any() and torch.equal(got[:, -300:], pk.fp8_linear(x, part))
