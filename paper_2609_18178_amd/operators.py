@@ -17,7 +17,7 @@ A training step of one linear layer::
     dx, dw = fp8_linear_backward(dy, w_t, columns, grad_weight=grad, accumulate=True)
 
 A small call's time is the host's: what is below reads each property of a tensor
-once and allocates once for what belongs together.
+once and allocates once for what lives and dies together.
 """
 from __future__ import annotations
 
@@ -150,7 +150,7 @@ class Fp8Matrix:
     rows are not contiguous (a transposed view, say) is copied into rows that are.
     """
 
-    __slots__ = ("rows", "cols", "_data", "_scale", "_room", "_at", "_index", "_bytes")
+    __slots__ = ("rows", "cols", "_data", "_scale", "_room", "_index", "_bytes")
 
     def __init__(self, data: torch.Tensor, scale: torch.Tensor, cols: int):
         if isinstance(data, _Tensor) and data.dim() == 2 and data.shape[1] > 1 and data.stride(1) != 1:
@@ -177,34 +177,34 @@ class Fp8Matrix:
                          torch.empty(rows, _pad(width // FP8_BLOCK, 4), dtype=torch.uint8, device=device), cols)
 
     @staticmethod
-    def _sizes(rows: int, cols: int) -> Tuple[int, int, int, int]:
-        """(bytes of a row, scales of a row, bytes of the rows, bytes of all) of one laid out by ``_carve``."""
+    def _sizes(rows: int, cols: int) -> Tuple[int, int, int]:
+        """(bytes of a row, scales of a row, where the scales start) in the room of one made by ``_new``."""
         width = (cols + 127) // 128 * 128
-        scales = (width // 128 + 3) // 4 * 4
-        data = (rows * width + 255) // 256 * 256
-        return width, scales, data, data + (rows * scales + 255) // 256 * 256
+        return width, (width // 128 + 3) // 4 * 4, (rows * width + 255) // 256 * 256
 
     @staticmethod
-    def _carve(room: torch.Tensor, at: int, base: int, rows: int, cols: int, sizes, index: int) -> "Fp8Matrix":
-        """One in the bytes of ``room`` (at address ``base``) from ``at`` on; its tensors are made when asked for."""
+    def _new(rows: int, cols: int, device, index: int) -> "Fp8Matrix":
+        """One of unspecified contents in an allocation of its own; its tensors are made when asked for."""
         m = Fp8Matrix.__new__(Fp8Matrix)
-        width, scales, data, _ = sizes
-        m.rows, m.cols, m._data, m._scale, m._room, m._at, m._index = rows, cols, None, None, room, at, index
-        m._bytes = _FP8.pack(base + at, base + at + data, rows, cols, width, scales)
+        width, scales, at = Fp8Matrix._sizes(rows, cols)
+        room = _empty(at + rows * scales, dtype=torch.uint8, device=device)
+        base = room.data_ptr()
+        m.rows, m.cols, m._data, m._scale, m._room, m._index = rows, cols, None, None, room, index
+        m._bytes = _FP8.pack(base, base + at, rows, cols, width, scales)
         return m
 
     @property
     def data(self) -> torch.Tensor:
         if self._data is None:
-            width, _, _, _ = self._sizes(self.rows, self.cols)
-            self._data = self._room.as_strided((self.rows, width), (width, 1), self._at)
+            width, _, _ = self._sizes(self.rows, self.cols)
+            self._data = self._room.as_strided((self.rows, width), (width, 1))
         return self._data
 
     @property
     def scale(self) -> torch.Tensor:
         if self._scale is None:
-            _, scales, data, _ = self._sizes(self.rows, self.cols)
-            self._scale = self._room.as_strided((self.rows, scales), (scales, 1), self._at + data)
+            _, scales, at = self._sizes(self.rows, self.cols)
+            self._scale = self._room.as_strided((self.rows, scales), (scales, 1), at)
         return self._scale
 
     @property
@@ -236,14 +236,12 @@ def fp8_quantize(x: torch.Tensor, along: str = "rows", square: bool = False,
     index = x.get_device()
     a = b = None
     if out is None:
-        first = Fp8Matrix._sizes(rows, cols) if along != "columns" else (0, 0, 0, 0)
-        second = Fp8Matrix._sizes(cols, rows) if along != "rows" else (0, 0, 0, 0)
-        room = _empty(first[3] + second[3], dtype=torch.uint8, device=x.device)
-        base = room.data_ptr()
+        # (each of its own: the columns are kept for the backward pass, and the rows' memory is free before it)
+        device = x.device
         if along != "columns":
-            a = Fp8Matrix._carve(room, 0, base, rows, cols, first, index)
+            a = Fp8Matrix._new(rows, cols, device, index)
         if along != "rows":
-            b = Fp8Matrix._carve(room, first[3], base, cols, rows, second, index)
+            b = Fp8Matrix._new(cols, rows, device, index)
     else:
         a, b = {"rows": (out, None), "columns": (None, out), "both": out}[along]
         for m, want in ((a, (rows, cols)), (b, (cols, rows))):

@@ -57,3 +57,14 @@ def test_more_columns_than_squares_of_16_in_a_launch():
     got = pk.fp8_linear(x, w)
     assert torch.equal(got, pk.fp8_matmul(pk.fp8_quantize(x), w))
     assert not got[:, :-300].any() and torch.equal(got[:, -300:], pk.fp8_linear(x, part))
+
+
+@pytest.mark.parametrize("kept", [0, 1])
+def test_either_of_a_pair_is_kept_without_the_other_s_memory(kept):
+    x = torch.zeros(2048, 4096, dtype=torch.bfloat16, device=DEV)
+    before = torch.cuda.memory_allocated()
+    held = pk.fp8_quantize(x, "both")[kept]
+    one = held.data.numel() + held.scale.numel()
+    assert one <= torch.cuda.memory_allocated() - before <= one + 4096
+    del held
+    assert torch.cuda.memory_allocated() == before
