@@ -70,8 +70,14 @@ _build/kernels-gfx950.s: $(PKG)/csrc/kernels.hip $(LIB_HDRS)
 	mkdir -p _build
 	$(HIPCC) $(filter-out -shared -fPIC,$(HIPFLAGS)) --cuda-device-only -S -o $@ $(PKG)/csrc/kernels.hip
 
+# the products' intermediate code, for the test of what is ordered in it
+ir: _build/fp8-gfx950.ll
+_build/fp8-gfx950.ll: $(PKG)/csrc/fp8.hip $(LIB_HDRS)
+	mkdir -p _build
+	$(HIPCC) $(filter-out -shared -fPIC,$(HIPFLAGS)) --cuda-device-only -S -emit-llvm -o $@ $<
+
 clean:
 	rm -f $(LIB) oracle/liboracle.so workloads/libgen.so $(C_CALLER) $(HW_APPROX)
 	rm -rf _build
 
-.PHONY: all clean isa
+.PHONY: all clean isa ir

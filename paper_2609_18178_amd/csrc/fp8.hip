@@ -858,6 +858,13 @@ struct TiledWide : Stage<BM, BN, WM, WN, kDeep> {
     }
 };
 
+// What the lanes of a wave have stored in LDS and what they read of each other's from here on, in that order (no
+// instruction: LDS serves a wave's in turn, the compiler has to keep them so).
+__device__ __forceinline__ void lanes_meet() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // LDS of a wave for what follows: 16 rows of its tile, a little more than their elements apart.
 template <int kFN>
 constexpr uint32_t kRowRoom = kFN * 64 + 16;
@@ -891,8 +898,7 @@ __device__ __forceinline__ void store_wave(const Product& p, uint32_t m, uint32_
                 *reinterpret_cast<v4f*>(in + j * 64 + g * 16) = acc[i][j];
             }
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        lanes_meet();
         if (half) {
 #pragma unroll
             for (uint32_t q = 0; q < kLanes16 / 4; ++q) {
@@ -918,8 +924,7 @@ __device__ __forceinline__ void store_wave(const Product& p, uint32_t m, uint32_
                 store4(p, m + i * 16 + k, n + q * 4, *reinterpret_cast<const v4f*>(room + k * kRowRoom<kFN> + q * 16));
             }
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        lanes_meet();
     }
 }
 
@@ -1135,6 +1140,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void shared_tile_kernel(const Produ
                 a.load_scales(k, p.kblocks, next_sa);
             }
         }
+        lanes_meet();
         v8i y[NT];
 #pragma unroll
         for (int j = 0; j < NT; ++j) y[j] = turn.get(room + j * 2048);
@@ -1146,6 +1152,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void shared_tile_kernel(const Produ
                 acc[i][j] = mfma_block<kWide>(y[j], x, acc[i][j], kWide ? sb[j] & 0xffu : sb[j], kWide ? sa[i] & 0xffu : sa[i]);
             }
         }
+        lanes_meet();
     }
     __syncthreads();
     v4f* sums = reinterpret_cast<v4f*>(lds);
@@ -1260,11 +1267,14 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(const Plain x,
                 const uint32_t k = first + u;
                 if ((uint32_t)u < runs.run && k < blocks) {
                     turn.put(room, line[u]);
+                    lanes_meet();
                     const uint8_t* a = held + (k * rows + row) * kBlockK;
                     const v8i xa = __builtin_shufflevector(*reinterpret_cast<const v4i*>(a + (g ^ swizzle(row)) * 16),
                                                            *reinterpret_cast<const v4i*>(a + ((g + 4) ^ swizzle(row)) * 16),
                                                            0, 1, 2, 3, 4, 5, 6, 7);
-                    acc = mfma_block<kWide>(turn.get(room), xa, acc, scales >> (8 * u) & 0xffu, held_scale[row * blocks + k]);
+                    const v8i xb = turn.get(room);
+                    lanes_meet();
+                    acc = mfma_block<kWide>(xb, xa, acc, scales >> (8 * u) & 0xffu, held_scale[row * blocks + k]);
                 }
             }
         }
