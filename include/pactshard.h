@@ -327,7 +327,9 @@ int pact_stream_probe_grid(const float* in0, const float* in1, const float* in2,
  * kernels on `stream` (and can be captured into a graph), argument errors are
  * found before anything is enqueued, and 0 or a PACT_E* code is returned.
  * Inputs of a call may overlap each other; an output may overlap nothing
- * (a gradient of the distillation loss may be the logits themselves).  Nothing
+ * (a gradient of the distillation loss may be the logits themselves; matrices
+ * whose rows are as far apart and lie beside each other, as column slices of a
+ * larger one do, do not overlap).  Nothing
  * depends on the order in which workgroups finish: the same call on the same
  * inputs gives the same bits, on every rank.
  * ------------------------------------------------------------------------ */

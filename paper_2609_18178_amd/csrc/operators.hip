@@ -34,7 +34,8 @@ uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 uint64_t round_up(uint64_t a, uint64_t b) { return ceil_div(a, b) * b; }
 uint32_t esize(uint32_t dtype) { return dtype == PACT_F32 ? 4 : 2; }
 
-// The buffers of one call. Inputs may share memory with each other, an output with nothing.
+// The buffers of one call. Inputs may share memory with each other, an output with nothing; rows of one matrix beside
+// those of another, as column slices of a larger one are, share none.
 class Spans {
 public:
     // rows x width bytes, `stride` bytes apart; false if that wraps the address space
@@ -43,13 +44,14 @@ public:
         const unsigned __int128 bytes = (unsigned __int128)(rows - 1) * stride + width;
         const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
         if (bytes > UINTPTR_MAX - lo) return false;
-        s_[n_++] = {lo, lo + (uintptr_t)bytes, written};
+        s_[n_++] = {lo, lo + (uintptr_t)bytes, rows > 1 ? stride : 0, width, written};
         return true;
     }
     bool overlap() const {
         for (int i = 0; i < n_; ++i) {
             for (int j = i + 1; j < n_; ++j) {
-                if ((s_[i].written || s_[j].written) && s_[i].lo < s_[j].hi && s_[j].lo < s_[i].hi) return true;
+                const Span &a = s_[i], &b = s_[j];
+                if ((a.written || b.written) && a.lo < b.hi && b.lo < a.hi && !beside(a, b)) return true;
             }
         }
         return false;
@@ -58,8 +60,17 @@ public:
 private:
     struct Span {
         uintptr_t lo, hi;
+        uint64_t stride, width;  // stride 0: one row
         bool written;
     };
+    // Whether no row of either meets one of the other, however many there are: the same distance between rows, and
+    // the one's bytes of it are not the other's. (A single row is taken to be one of rows so far apart.)
+    static bool beside(const Span& a, const Span& b) {
+        const uint64_t stride = a.stride != 0 ? a.stride : b.stride;
+        if (stride == 0 || (b.stride != 0 && b.stride != stride)) return false;
+        const uint64_t ahead = b.lo >= a.lo ? (b.lo - a.lo) % stride : (stride - (a.lo - b.lo) % stride) % stride;
+        return ahead >= a.width && b.width <= stride && ahead <= stride - b.width;
+    }
     Span s_[10];
     int n_ = 0;
 };

@@ -68,3 +68,23 @@ def test_either_of_a_pair_is_kept_without_the_other_s_memory(kept):
     assert one <= torch.cuda.memory_allocated() - before <= one + 4096
     del held
     assert torch.cuda.memory_allocated() == before
+
+
+def test_input_and_output_as_slices_of_one_matrix():
+    w = _weight(70, 203)
+    for rows in (3, 200):
+        x = torch.randn(rows, 203, generator=_gen(rows)).to(DEV)
+        room = torch.full((rows, 300), 5.0, device=DEV)
+        room[:, 11:214] = x
+        pk.fp8_linear(room[:, 11:214], w, out=room[:, 214:284])
+        assert torch.equal(room[:, 214:284], pk.fp8_linear(x, w, dtype=torch.float32)) and torch.equal(room[:, 11:214], x)
+        assert (room[:, :11] == 5).all() and (room[:, 284:] == 5).all()
+    logits = torch.randn(40, 1003, generator=_gen(5)).bfloat16().to(DEV)
+    top, index = torch.topk(logits.float(), 8, 1)
+    room = torch.zeros(40, 2006, dtype=torch.bfloat16, device=DEV)
+    room[:, 1003:] = logits
+    loss, grad = pk.distill_step(logits, top, index, 2.0)
+    assert torch.equal(pk.distill_step(room[:, 1003:], top, index, 2.0, grad=room[:, :1003])[0], loss)
+    assert torch.equal(room[:, :1003], grad) and torch.equal(room[:, 1003:], logits)
+    with pytest.raises(pk.PactError):
+        pk.distill_step(room[:, 1003:], top, index, 2.0, grad=room[:, 1:1004])
