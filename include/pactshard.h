@@ -436,7 +436,9 @@ int pact_fp8_linear_backward(const pact_matrix* dy, const pact_fp8* w_cols, cons
  * entry) has q = 0; the loss is +infinity where the teacher gives it any
  * probability.  A NaN among the logits that count makes its row NaN, and so
  * does an index of `vocab` or more (masked entries keep a zero gradient).
- * Probabilities, sums and losses are binary32; grad has the logits' type. */
+ * Probabilities, sums and losses are binary32; grad has the logits' type.  The
+ * order of a row's sums follows where it starts in its 16 bytes: the same bits
+ * need logits that are laid out alike. */
 #define PACT_DISTILL_MAX_TOP 1024
 typedef struct pact_distill {
     const void* logits;      /* rows x vocab, dtype                            */
