@@ -16,6 +16,11 @@ A training step of one linear layer::
     ...
     dx, dw = fp8_linear_backward(dy, w_t, columns, grad_weight=grad, accumulate=True)
 
+The calls are outside of autograd: a result has no graph, whatever its inputs require, and
+gradients are what ``fp8_linear_backward`` and ``distill_grad`` or ``distill_step`` return
+(an ``autograd.Function`` can be made of them). What is written into a tensor that a caller
+hands over (``out``, ``grad``, ``grad_weight``) counts for autograd as changed in place.
+
 A small call's time is the host's: what is below reads each property of a tensor
 once and allocates once for what lives and dies together.
 """
@@ -50,6 +55,7 @@ _INDEX = {torch.int32: 4, torch.int64: 8}
 
 _Tensor = torch.Tensor
 _empty = torch.empty
+_changed = torch.autograd.graph.increment_version
 _current_device = torch._C._cuda_getDevice
 _raw_stream = torch._C._cuda_getCurrentRawStream
 
@@ -249,6 +255,10 @@ def fp8_quantize(x: torch.Tensor, along: str = "rows", square: bool = False,
                 raise ValueError(f"out is {m.shape}, the result is {want}")
     _run("pact_fp8_quantize", index, _MATRIX.pack(x.data_ptr(), rows, cols, ld, kind, 0), None if a is None else a._bytes,
          None if b is None else b._bytes, _FLAG_SQUARE if square else 0)
+    if out is not None:
+        for m in (a, b):
+            if m is not None:
+                _changed((m._data, m._scale) if m._room is None else m._room)
     return (a, b) if along == "both" else b if a is None else a
 
 
@@ -279,9 +289,12 @@ def fp8_matmul(a: Fp8Matrix, b: Fp8Matrix, out: Optional[torch.Tensor] = None, d
     m, n, k = a.rows, b.rows, a.cols
     if k != b.cols:
         raise ValueError(f"a has {k} columns and b {b.cols}")
+    given = out is not None
     out, packed = _result(out, m, n, dtype, a, index, accumulate)
     _keep, at, nbytes = _scratch("pact_fp8_matmul_workspace_bytes", m, n, k, a)
     _run("pact_fp8_matmul", index, a._bytes, b._bytes, packed, _FLAG_ACCUMULATE if accumulate else 0, at, nbytes)
+    if given:
+        _changed(out)
     return out
 
 
@@ -292,9 +305,12 @@ def fp8_linear(x: torch.Tensor, w: Fp8Matrix, out: Optional[torch.Tensor] = None
     n = _fp8(w, "w", index).rows
     if cols != w.cols:
         raise ValueError(f"x has {cols} columns and w {w.cols}")
+    given = out is not None
     out, packed = _result(out, rows, n, dtype, x, index)
     _keep, at, nbytes = _scratch("pact_fp8_linear_workspace_bytes", rows, n, cols, x)
     _run("pact_fp8_linear", index, _MATRIX.pack(x.data_ptr(), rows, cols, ld, kind, 0), w._bytes, packed, at, nbytes)
+    if given:
+        _changed(out)
     return out
 
 
@@ -321,6 +337,8 @@ def fp8_linear_backward(dy: torch.Tensor, w_columns: Fp8Matrix, x_columns: Fp8Ma
     _keep, at, nbytes = _scratch("pact_fp8_linear_backward_workspace_bytes", m, n, k, dy)
     _run("pact_fp8_linear_backward", index, _MATRIX.pack(dy.data_ptr(), m, n, ld, kind, 0), w_columns._bytes,
          x_columns._bytes, dx_packed, dw_packed, _FLAG_ACCUMULATE if accumulate else 0, at, nbytes)
+    if grad_weight is not None:
+        _changed(dw)
     return dx, dw
 
 
@@ -351,6 +369,7 @@ def _distill(name: str, logits, top_logits, top_index, temperature, row_weight, 
         if keep_lse:  # (of its own: parting one allocation costs more than a second)
             lse = _empty(rows, dtype=torch.float32, device=logits.device)
             lse_at = lse.data_ptr()
+    given = None
     if grad is None:
         grad = _empty(rows, vocab, dtype=logits.dtype, device=logits.device)
         grad_at, grad_ld = grad.data_ptr(), vocab
@@ -358,7 +377,7 @@ def _distill(name: str, logits, top_logits, top_index, temperature, row_weight, 
         g_rows, g_cols, grad_ld, g_kind = _matrix(grad, "grad", index)
         if g_rows != rows or g_cols != vocab or g_kind != kind:
             raise ValueError(f"grad must be {logits.dtype} of {tuple(logits.shape)}")
-        grad_at = grad.data_ptr()
+        grad_at, given = grad.data_ptr(), grad
     packed = _DISTILL.pack(logits.data_ptr(), grad_at, top_logits.data_ptr(), top_index.data_ptr(), weight_at, loss_at,
                            lse_at, rows, vocab, top, ld, grad_ld, t_ld, i_ld, temperature, kind, t_kind, i_bytes, 0,
                            _raw_stream(index))
@@ -370,6 +389,8 @@ def _distill(name: str, logits, top_logits, top_index, temperature, row_weight, 
             rc = f(packed)
     if rc != PACT_OK:
         raise PactError(rc, name)
+    if given is not None:
+        _changed(given)
     return loss, lse, grad
 
 

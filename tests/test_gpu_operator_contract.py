@@ -89,3 +89,37 @@ def test_input_and_output_as_slices_of_one_matrix():
     assert torch.equal(room[:, :1003], grad) and torch.equal(room[:, 1003:], logits)
     with pytest.raises(pk.PactError):
         pk.distill_step(room[:, 1003:], top, index, 2.0, grad=room[:, 1:1004])
+
+
+def test_autograd_sees_what_is_written_in_place_and_results_have_no_graph():
+    x = torch.randn(20, 130, generator=_gen(1)).to(DEV).requires_grad_()
+    w = _weight(60, 130)
+    top, index = torch.randn(20, 4, device=DEV), torch.zeros(20, 4, dtype=torch.int32, device=DEV)
+    wt, xt = pk.fp8_quantize(torch.zeros(60, 130, device=DEV), "columns"), pk.fp8_quantize(x, "columns")
+    y = pk.fp8_linear(x, w, dtype=torch.float32)
+    assert not y.requires_grad and not pk.distill_step(x, top, index)[1].requires_grad
+
+    def written(t):
+        """An output of exp, which its backward pass reads, and the tensor that a call writes (of the same memory)."""
+        z = torch.exp(t.requires_grad_())
+        return z, z.detach()
+
+    dy, lse = torch.zeros(20, 60, device=DEV), torch.zeros(20, device=DEV)
+    for like, call in ((y, lambda out: pk.fp8_linear(x, w, out=out)),
+                       (y, lambda out: pk.fp8_matmul(pk.fp8_quantize(x), w, out=out)),
+                       (torch.zeros(60, 130, device=DEV), lambda out: pk.fp8_linear_backward(dy, wt, xt, grad_weight=out)),
+                       (x.detach(), lambda out: pk.distill_step(out, top, index, grad=out)),
+                       (x.detach(), lambda out: pk.distill_grad(x, top, index, lse, grad=out))):
+        z, out = written(like.clone())
+        z.sum().backward()                  # (without a call nothing is wrong)
+        z, out = written(like.clone())
+        call(out)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            z.sum().backward()
+    held = pk.fp8_quantize(x)
+    for m in (held, pk.Fp8Matrix(held.data.clone(), held.scale.clone(), 130)):
+        before = m.data._version, m.scale._version
+        pk.fp8_quantize(x, out=m)
+        assert m.data._version > before[0] and m.scale._version > before[1]
+    with torch.inference_mode():            # (tensors that keep no count)
+        pk.fp8_linear(x, w, out=torch.empty(20, 60, device=DEV))
