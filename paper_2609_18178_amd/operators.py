@@ -32,7 +32,7 @@ from typing import Optional, Tuple, Union
 
 import torch
 
-from . import PACT_OK, PactError, _lib
+from . import PACT_EINVAL, PACT_OK, PactError, _lib
 
 __all__ = [
     "Fp8Matrix", "fp8_quantize", "fp8_matmul", "fp8_linear", "fp8_linear_backward",
@@ -330,8 +330,8 @@ def fp8_linear_backward(dy: torch.Tensor, w_columns: Fp8Matrix, x_columns: Fp8Ma
         raise ValueError(f"dy has {m} rows and x {x_columns.cols}")
     if w_columns.cols != n or w_columns.rows != k:
         raise ValueError(f"w_columns is {w_columns.shape}, not {(k, n)}")
-    if grad_weight is not None and grad_weight.dtype is not torch.float32:
-        raise TypeError("grad_weight must be float32")
+    if grad_weight is not None and (not isinstance(grad_weight, _Tensor) or grad_weight.dtype is not torch.float32):
+        raise TypeError("grad_weight must be a float32 tensor")
     dw, dw_packed = _result(grad_weight, n, k, torch.float32, dy, index, accumulate)
     dx, dx_packed = _result(None, m, k, dy.dtype, dy, index) if need_dx else (None, None)
     _keep, at, nbytes = _scratch("pact_fp8_linear_backward_workspace_bytes", m, n, k, dy)
@@ -378,9 +378,14 @@ def _distill(name: str, logits, top_logits, top_index, temperature, row_weight, 
         if g_rows != rows or g_cols != vocab or g_kind != kind:
             raise ValueError(f"grad must be {logits.dtype} of {tuple(logits.shape)}")
         grad_at, given = grad.data_ptr(), grad
-    packed = _DISTILL.pack(logits.data_ptr(), grad_at, top_logits.data_ptr(), top_index.data_ptr(), weight_at, loss_at,
-                           lse_at, rows, vocab, top, ld, grad_ld, t_ld, i_ld, temperature, kind, t_kind, i_bytes, 0,
-                           _raw_stream(index))
+    try:
+        packed = _DISTILL.pack(logits.data_ptr(), grad_at, top_logits.data_ptr(), top_index.data_ptr(), weight_at, loss_at,
+                               lse_at, rows, vocab, top, ld, grad_ld, t_ld, i_ld, temperature, kind, t_kind, i_bytes, 0,
+                               _raw_stream(index))
+    except struct.error:
+        raise TypeError(f"temperature must be a number, not {temperature!r}") from None
+    except OverflowError:  # (beyond binary32, as infinity is)
+        raise PactError(PACT_EINVAL, name) from None
     f = getattr(_lib(), name)
     if _current_device() == index:
         rc = f(packed)

@@ -123,3 +123,18 @@ def test_autograd_sees_what_is_written_in_place_and_results_have_no_graph():
         assert m.data._version > before[0] and m.scale._version > before[1]
     with torch.inference_mode():            # (tensors that keep no count)
         pk.fp8_linear(x, w, out=torch.empty(20, 60, device=DEV))
+
+
+def test_refusals_name_the_argument():
+    x = torch.zeros(6, 130, device=DEV)
+    top, index = x[:, :4].contiguous(), torch.zeros(6, 4, device=DEV, dtype=torch.int32)
+    xt = pk.fp8_quantize(x, "columns")
+    wt = pk.fp8_quantize(torch.zeros(9, 130, device=DEV), "columns")
+    with pytest.raises(TypeError, match="grad_weight"):
+        pk.fp8_linear_backward(x[:, :9].contiguous(), wt, xt, grad_weight=[0.0])
+    for bad in (None, "1", top):
+        with pytest.raises(TypeError, match="temperature"):
+            pk.distill_loss(x, top, index, temperature=bad)
+    for bad in (1e39, -1e39, float("inf")):
+        with pytest.raises(pk.PactError):
+            pk.distill_step(x, top, index, temperature=bad)
