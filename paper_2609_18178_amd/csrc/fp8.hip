@@ -386,7 +386,9 @@ __global__ __launch_bounds__(256) void transpose_kernel(const Bytes b) {
 // 2-norm at any K for normally distributed elements (the 8-bit instructions without scales
 // likewise), a hundredth of what rounding to bf16 costs. Where C is binary32 the bytes are
 // therefore widened to bf16 with their scale, exactly, and go through the bf16 instruction at
-// half the rate, whose sums are binary32: 8e-8 off at K = 4096.
+// half the rate, whose sums are binary32: 8e-8 off at K = 4096.  (Exactly where bf16 has the number: scale
+// bytes of 3 to 246. Beside those the least bits of an element end at 2^-133, and 2^128 is infinite; the scaled
+// instruction takes every scale.)
 // ---------------------------------------------------------------------------
 template <int Sb, int Sa>
 __device__ __forceinline__ v4f mfma(v8i b, v8i a, v4f c, uint32_t scale_b, uint32_t scale_a) {

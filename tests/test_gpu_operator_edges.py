@@ -64,3 +64,45 @@ def test_teacher_logits_at_the_ends_of_their_type(top, temperature, dtype):
         size[at] += p
         for got in (alone, grad.cpu().double()):
             assert bool(((got[r] - want_grad).abs() <= 2 * near * size / temperature + 1e-37).all()), r
+
+
+# ---------------------------------------------------------------------------
+# scales of every size
+# ---------------------------------------------------------------------------
+
+CODES = [0x01, 0x03, 0x08, 0x38, 0x7E, 0xF8]  # 2^-9, 3 * 2^-9, 2^-6, 1, 448, -256
+
+
+def _one_element_rows(times=1):
+    """A row for each scale byte and code, of one element; and the elements in 64 bits."""
+    data = torch.zeros(255 * len(CODES), 128, dtype=torch.uint8)
+    data[:, 0] = torch.tensor(CODES, dtype=torch.uint8).repeat(255)
+    scale = torch.zeros(255 * len(CODES), 4, dtype=torch.uint8)
+    scale[:, 0] = torch.arange(255, dtype=torch.int32).repeat_interleave(len(CODES)).to(torch.uint8)
+    a = pk.Fp8Matrix(data.repeat(times, 1).to(DEV), scale.repeat(times, 1).to(DEV), 128)
+    return a, torch.from_numpy(ref.stands_for(a.data, a.scale, 128))[:, 0], a.scale[:, 0].cpu().int()
+
+
+# squares of 16, 32 and 64 whose waves share K, then of 128, then of 256
+@pytest.mark.parametrize("rows,times", [(12, 1), (100, 1), (500, 1), (1530, 1), (4590, 3)])
+def test_products_over_all_scales(rows, times):
+    """One product a result, so that each is its rounding: with bf16 result whatever the scales, with binary32 result
+    where both scale bytes are from 3 to 246. Outside, the operand's bf16 number is off by half of 2^-133 at most, and an
+    element of 2^128 or more is infinite there."""
+    print("scales", rows, times, flush=True)
+    b, y, sb = _one_element_rows(times)
+    for first in sorted({0, min(700, len(y) - rows), len(y) - rows}):
+        a = pk.Fp8Matrix(b.data[first:first + rows], b.scale[first:first + rows], 128)
+        x, sa = y[first:first + rows], sb[first:first + rows]
+        want = x[:, None] * y[None, :]
+        got = pk.fp8_matmul(a, b).cpu()
+        assert torch.equal(got, want.float().bfloat16())
+        got = pk.fp8_matmul(a, b, dtype=torch.float32).cpu()
+        within = ((sa >= 3) & (sa <= 246))[:, None] & ((sb >= 3) & (sb <= 246))[None, :]
+        assert torch.equal(got[within], want.float()[within])
+        infinite = (x.abs() >= 2.0 ** 128)[:, None] | (y.abs() >= 2.0 ** 128)[None, :]
+        assert not bool(got[infinite].isfinite().any())                 # (NaN: times an element that is zero there)
+        low = ~within & ~infinite & (want.abs() < 2.0 ** 127)
+        off = (got.double() - want).abs()
+        held = 2.0 ** -134 * (x.abs()[:, None] + y.abs()[None, :] + 2.0 ** -134) + 2.0 ** -149
+        assert bool((off <= held)[low].all())
