@@ -182,25 +182,28 @@ Parts parts_of(uint64_t m, uint64_t n, uint64_t k) {
 // its rows on the way, so that both give the same bits, and the larger squares would be empty in most of their rows.  us, weights out of
 // memory, in the larger squares / of 16, with bf16 and with binary32 result: 1 x 17000 x 4096 23.3 / 16.4, 30.9 / 16.3; 1 x 140000 x 4096 148 / 93,
 // 165 / 94; 16 x 140000 x 4096 154 / 114, 171 / 121; 1 x 140000 x 520 30.1 / 28.3, 36.3 / 33.2; 1 x 65536 x 520 13.3 / 14.9, 16.2 / 17.6.
-// us per product of inputs out of memory, in squares of 16 / 32 / 64 / 128, deep / 128 / 256:
-//                 K = 1024                                  K = 4096
-//     16 x  4096   4.2   5.7   9.7    -  16.9  41     (K = 4096, inputs in cache)
-//     64 x  4096   5.1   4.7   6.8   8.0   9.4  15.0  12.1   9.2  15.7  20.0  32.8  49.6
-//    128 x  4096   7.9   5.7   6.9   7.5   9.0  15.0  19.3  13.1  15.4  23.2  33.9  50.5
-//    256 x  4096  13.1   9.1   7.2   7.6   9.0  14.5  33.3  20.3  15.0  22.7  33.7  54.1
-//    512 x  4096    -   16.6   9.5   8.3  10.0  15.2    -   35.4  22.9  22.7  33.6  53.3
-//   1024 x  4096    -   30.0  16.9  10.0  10.5  15.7    -   63.7  39.0  23.9  33.9  52.1
-//    512 x 14336    -     -   29.7  18.7  15.3  19.4    -     -   66.6  45.3  41.3  53.1
-//   2500 x  4096    -     -   35.5  24.3  21.9  20.5    -     -   82.0  57.7  59.9  52.0
-//   4096 x  4096    -     -   57.4  34.1  29.5  22.7    -     -   136   88.3  78.4  60.2
-//  14336 x  4096    -     -     -    100  85.3  79.0    -     -     -    269   243   206
+// us per product of inputs out of memory, in squares of 16 / 32 / 64 / 128, deep / 128 / 256, with bf16 result:
+//                 K = 1024                               K = 4096
+//     16 x  4096    4.3   4.9   7.0   8.8     -     -     6.8   8.2  13.0  18.3     -     -
+//     64 x  4096    6.1   5.2   8.1   8.9     -     -    11.9   9.0  15.4  19.9     -     -
+//    128 x  4096    9.4   6.6   7.9   9.2     -     -    18.7  12.5  15.0  22.9     -     -
+//    256 x  4096   15.1  10.6   8.1   9.2  11.7     -    33.0  19.9  14.8  22.6  33.9     -
+//    512 x  4096      -  18.2  10.2   9.5  11.9  16.2       -  33.8  22.1  22.7  33.8  43.1
+//   1024 x  4096      -  33.5  17.7  10.8  12.7  16.7       -  59.6  36.4  24.4  34.6  43.0
+//    512 x 14336      -     -  29.5  19.2  16.0  18.4       -     -  62.6  47.4  42.7  46.3
+//   2500 x  4096      -     -  34.9  24.6  22.4  19.6       -     -  78.5  58.7  60.9  47.3
+//   4096 x  4096      -     -  55.8  35.0  29.3  22.5       -     -   125  88.8  77.3  56.6
+//   6000 x  4096      -     -     -  48.2  40.0  39.3       -     -     -   116   103  97.6
+//  14336 x  4096      -     -     -  99.3  78.3  78.3       -     -     -   261   232   200
 // and with binary32 result:
-//    512 x  4096    -   18.5  13.3  13.0  14.3  28.4    -   38.5  32.1  35.4  46.7  94.3
-//   1024 x  4096    -   31.7  22.3  14.5  16.0  29.4    -   72.5  58.8  37.9  48.6  94.7
-//   2500 x  4096    -     -   48.4  36.4  31.0  35.0    -     -   124   101   92.3  96.8
-//   4096 x  4096    -     -   79.1  52.9  42.9  37.2    -     -   197   148   121   108
-//   6000 x  4096    -     -     -   73.4  59.0  68.1    -     -     -   203   174   188
-//  14336 x  4096    -     -     -    160   128   129    -     -     -    469   401   374
+//    256 x  4096   18.8  11.7  10.2  12.7  15.7     -    36.9  22.0  23.6  33.6  46.5     -
+//    512 x  4096      -  19.9  14.0  13.3  16.2  28.0       -  38.8  32.3  34.7  47.1  81.9
+//   1024 x  4096      -  35.7  23.6  15.1  17.6  29.0       -  66.3  54.3  36.6  46.9  81.8
+//    512 x 14336      -     -  39.8  26.7  20.8  30.0       -     -  97.1  71.3  58.8  84.5
+//   2500 x  4096      -     -  45.9  36.5  31.7  33.6       -     -   120  99.9  91.1  90.1
+//   4096 x  4096      -     -  76.8  52.4  41.9  36.6       -     -   195   138   117  99.0
+//   6000 x  4096      -     -     -  71.1  59.7  66.3       -     -     -   201   168   179
+//  14336 x  4096      -     -     -   154   123   124       -     -     -   468   398   361
 Cut cut(uint64_t m, uint64_t n, uint64_t k, bool wide) {
     auto tiles = [&](uint64_t side) { return ceil_div(m, side) * ceil_div(n, side); };
     const Parts parts = parts_of(m, n, k);
@@ -223,17 +226,20 @@ Cut cut(uint64_t m, uint64_t n, uint64_t k, bool wide) {
 // the turns that are full (to seven eighths), then the rest, of at most 512 squares of 128, in a launch of its own: one
 // deep square a CU, or two.  That saves a part of a turn: K has to be long, and for a binary32 result, whose squares
 // of 128 wait for less, longer where only one turn is full; and the second launch has to be well filled.
-// us uncut / cut, inputs out of memory, with bf16 and with binary32 result:
-//                       K = 1024                    K = 2048                    K = 4096
-//    4300 x  4096   27.9 / 26.9   40.9 / 46.1   50.8 / 42.9   72.5 / 74.3   82.3 / 66.8    130 / 126
-//    5000 x  4096   28.9 / 27.7   42.2 / 46.8   46.7 / 40.5   71.4 / 73.3   83.8 / 68.5    134 / 128
-//    6000 x  4096   31.8 / 32.3   47.8 / 53.5   50.7 / 48.5   83.0 / 84.1   87.2 / 81.8    156 / 148
-//    1300 x 14336     -             -             -             -           82.9 / 72.4    132 / 143
-//    3000 x 11008   45.6 / 41.2   68.6 / 76.0   75.2 / 63.9    120 / 121     133 / 110     228 / 216
-//    8192 x  4800     -             -             -             -            136 / 125     280 / 237
-//    8192 x  5120   45.4 / 45.0   90.9 / 88.3   74.0 / 72.5    153 / 140     135 / 129     293 / 243
-//   14336 x  4096   62.0 / 62.8    111 / 118     100 / 102     198 / 190     187 / 184     362 / 338
-//    8192 x  8900     -             -             -             -            260 / 254     474 / 442
+// Of two ways to cut, rows of C or its columns, the one that leaves more squares to the second launch (8192 x 4800 x 4096 by
+// rows / columns 145 / 147 us and 245 / 243, 8192 x 8900 x 4096 258 / 258 and 443 / 443).
+// us uncut / cut, inputs out of memory, with bf16 and with binary32 result (within 3%; for K = 1024 and one turn of a binary32 result
+// of K = 2048, 1300 x 14336 x 4096 among them, the cut that the rule does not make):
+//                       K = 1024                     K = 2048                     K = 4096
+//   4300 x  4096   34.6 / 32.0   49.9 / 50.4   52.8 / 46.8   79.9 / 77.9   89.8 / 77.0    142 /  130
+//   5000 x  4096   35.4 / 33.3   49.2 / 54.7   53.0 / 48.5   79.6 / 83.3   91.5 / 80.7    144 /  136
+//   6000 x  4096   38.8 / 39.6   55.3 / 59.2   57.8 / 57.8   94.5 / 95.6   97.3 / 95.6    174 /  158
+//   1300 x 14336   37.6 / 34.9   54.0 / 52.8   56.8 / 51.7   85.0 / 85.7   94.0 / 86.2    156 /  148
+//   3000 x 11008   55.8 / 51.5   77.4 / 82.2   83.0 / 75.3    132 /  125    141 /  127    240 /  216
+//   8192 x  4800   60.1 / 58.2    100 / 90.7   88.3 / 85.7    158 /  141    148 /  146    281 /  243
+//   8192 x  5120   58.7 / 57.8   99.1 / 92.8   87.1 / 86.7    159 /  144    151 /  148    289 /  249
+//  14336 x  4096   78.5 / 79.8    126 /  129    118 /  119    200 /  196    195 /  199    364 /  351
+//   8192 x  8900    109 /  104    188 /  166    157 /  153    267 /  253    259 /  258    460 /  437
 struct Split {
     bool rows;    // of C, or its columns
     uint64_t at;  // where; 0: not cut
