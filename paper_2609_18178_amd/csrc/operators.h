@@ -84,7 +84,7 @@ struct DistillArgs {
     uint64_t ld_logits, ld_grad, ld_top_logits, ld_top_index;  // elements
     uint32_t rows, vocab, top;
     float to_log2;            // log2(e) / temperature
-    float inv_temperature, temperature;
+    float inv_temperature;
     uint32_t dtype, top_dtype;
     bool wide_index;          // 64-bit indices
 };

@@ -411,7 +411,6 @@ int distill(pact::Distill kind, const pact_distill* s) {
     d.rows = (uint32_t)s->rows;
     d.vocab = (uint32_t)s->vocab;
     d.top = (uint32_t)s->top;
-    d.temperature = s->temperature;
     d.inv_temperature = (float)(1.0 / (double)s->temperature);
     d.to_log2 = to_log2;
     d.dtype = s->dtype;
