@@ -325,13 +325,12 @@ int pact_stream_probe_grid(const float* in0, const float* in1, const float* in2,
  *
  * As above: every buffer is the caller's device memory, a call only enqueues
  * kernels on `stream` (and can be captured into a graph), argument errors are
- * found before anything is enqueued, and 0 or a PACT_E* code is returned.
- * Inputs of a call may overlap each other; an output may overlap nothing
- * (a gradient of the distillation loss may be the logits themselves; matrices
- * whose rows are as far apart and lie beside each other, as column slices of a
- * larger one do, do not overlap).  Nothing
- * depends on the order in which workgroups finish: the same call on the same
- * inputs gives the same bits, on every rank.
+ * found before anything is enqueued, and 0 or a PACT_E* code is returned. Inputs
+ * of a call may overlap each other; an output may overlap nothing (a gradient of
+ * the distillation loss may be the logits themselves; matrices whose rows are as
+ * far apart and lie beside each other, as column slices of a larger one do, do
+ * not overlap).  Nothing depends on the order in which workgroups finish: the
+ * same call on the same inputs gives the same bits, on every rank.
  * ------------------------------------------------------------------------ */
 
 /* Element types of a matrix. */
@@ -386,19 +385,21 @@ int pact_fp8_transpose(const uint8_t* in, uint64_t rows, uint64_t cols, uint64_t
 
 /* c[i, j] = sum over k of a[i, k] * b[j, k]: a is m x k, b is n x k, c is m x n
  * of either type.  Where c is binary32 the products are exact and their sums
- * binary32, of elements that bf16 holds: all that have a scale byte of 3 ... 246.
- * With a smaller one (blocks of numbers below 1e-35) an element is off by up to
- * 2^-134, and one of 2^128 or more (a number from 3.29e38 on is rounded to that)
- * is infinite.  Where c is bf16 every scale is exact; the products go through the 8-bit matrix instruction,
- * which holds the sum of a block of 128 in fewer than 24 bits (off by less than
- * 2^-15 of the sum of the products' sizes), adds the blocks in binary32, and
- * the result is rounded once.  PACT_FP8_ACCUMULATE: c, binary32, is added to (gradients
- * over several microbatches).  Forward: a = x, b = W.  Gradient of the input:
- * a = dy, b = W along its columns.  Gradient of the weight: a = dy and b = x,
- * both along their columns.  Where c is small and k long, parts of k are summed
- * beside each other in the workspace and then joined, always in the same order.
- * workspace: pact_fp8_matmul_workspace_bytes(m, n, k) bytes, often none (256-byte
- * aligned; PACT_EINVAL if it is smaller). */
+ * binary32, of elements that bf16 holds: all that have a scale byte of 3 ...
+ * 246. With a smaller one (blocks of numbers below 1e-35) an element is off by
+ * up to 2^-134, and one of 2^128 or more (a number from 3.29e38 on is rounded to
+ * that) is infinite.  Where c is bf16 every scale is exact; the products go
+ * through the 8-bit matrix instruction, which holds the sum of a block of 128 in
+ * fewer than 24 bits (off by less than 2^-15 of the sum of the products' sizes),
+ * adds the blocks in binary32, and the result is rounded once.
+ * PACT_FP8_ACCUMULATE: c, binary32, is added to (gradients over several
+ * microbatches).  Forward: a = x, b = W.  Gradient of the input: a = dy, b = W
+ * along its columns.  Gradient of the weight: a = dy and b = x, both along their
+ * columns.  Where c is small and k long, parts of k are summed beside each other
+ * in the workspace and then joined, always in the same order. workspace:
+ * pact_fp8_matmul_workspace_bytes(m, n, k) bytes, often none (256-byte aligned;
+ * PACT_EINVAL if it is smaller): what a result of either type may take, of which
+ * one of bf16 may leave all alone. */
 #define PACT_FP8_ACCUMULATE 1u
 int64_t pact_fp8_matmul_workspace_bytes(uint64_t m, uint64_t n, uint64_t k);
 int pact_fp8_matmul(const pact_fp8* a, const pact_fp8* b, const pact_matrix* c, uint32_t flags, void* workspace,

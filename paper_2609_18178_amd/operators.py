@@ -55,7 +55,7 @@ _INDEX = {torch.int32: 4, torch.int64: 8}
 
 _Tensor = torch.Tensor
 _empty = torch.empty
-_changed = torch.autograd.graph.increment_version
+_changed = torch._C._increment_version  # (torch.autograd.graph.increment_version at a third of its time)
 _current_device = torch._C._cuda_getDevice
 _raw_stream = torch._C._cuda_getCurrentRawStream
 
@@ -234,7 +234,7 @@ def fp8_quantize(x: torch.Tensor, along: str = "rows", square: bool = False,
                  out: Union[None, Fp8Matrix, Tuple[Fp8Matrix, Fp8Matrix]] = None):
     """``x`` (rows x cols, float32 or bfloat16) in FP8: ``along`` its "rows" (rows x cols), its
     "columns" (the transposed matrix with its own scales, cols x rows), or "both" in one pass, as
-    a pair.  ``square``: one scale for each 128 x 128 square (weights).  ``out``: matrices of the
+    a pair, each in memory of its own.  ``square``: one scale for each 128 x 128 square (weights).  ``out``: matrices of the
     result's shape to write instead of new ones."""
     rows, cols, ld, kind = _matrix(x, "x")
     if along not in ("rows", "columns", "both"):
@@ -258,7 +258,7 @@ def fp8_quantize(x: torch.Tensor, along: str = "rows", square: bool = False,
     if out is not None:
         for m in (a, b):
             if m is not None:
-                _changed((m._data, m._scale) if m._room is None else m._room)
+                _changed((m._data, m._scale) if m._room is None else (m._room,))
     return (a, b) if along == "both" else b if a is None else a
 
 
@@ -283,7 +283,9 @@ def _result(out: Optional[torch.Tensor], rows: int, cols: int, dtype, like, inde
 def fp8_matmul(a: Fp8Matrix, b: Fp8Matrix, out: Optional[torch.Tensor] = None, dtype=torch.bfloat16,
                accumulate: bool = False) -> torch.Tensor:
     """``a @ b.T`` of two FP8 matrices that are quantised along the columns they share: m x n
-    elements of ``dtype``, or of ``out``'s; ``accumulate`` adds to ``out`` (float32)."""
+    elements of ``dtype``, or of ``out``'s; ``accumulate`` adds to ``out`` (float32).  Sums of a
+    float32 result are binary32; those of a bfloat16 one are the 8-bit instruction's, a hundredth of
+    the result's rounding off."""
     index = _fp8(a, "a")._index
     _fp8(b, "b", index)
     m, n, k = a.rows, b.rows, a.cols
@@ -294,7 +296,7 @@ def fp8_matmul(a: Fp8Matrix, b: Fp8Matrix, out: Optional[torch.Tensor] = None, d
     _keep, at, nbytes = _scratch("pact_fp8_matmul_workspace_bytes", m, n, k, a)
     _run("pact_fp8_matmul", index, a._bytes, b._bytes, packed, _FLAG_ACCUMULATE if accumulate else 0, at, nbytes)
     if given:
-        _changed(out)
+        _changed((out,))
     return out
 
 
@@ -310,7 +312,7 @@ def fp8_linear(x: torch.Tensor, w: Fp8Matrix, out: Optional[torch.Tensor] = None
     _keep, at, nbytes = _scratch("pact_fp8_linear_workspace_bytes", rows, n, cols, x)
     _run("pact_fp8_linear", index, _MATRIX.pack(x.data_ptr(), rows, cols, ld, kind, 0), w._bytes, packed, at, nbytes)
     if given:
-        _changed(out)
+        _changed((out,))
     return out
 
 
@@ -319,6 +321,7 @@ def fp8_linear_backward(dy: torch.Tensor, w_columns: Fp8Matrix, x_columns: Fp8Ma
                         need_dx: bool = True) -> Tuple[Optional[torch.Tensor], torch.Tensor]:
     """The gradients of ``y = x W^T`` from ``dy`` (rows x n): ``(dx, dw)`` with ``dx = dy W`` in dy's
     type and ``dw = dy^T x`` in float32, written or (``accumulate``) added to ``grad_weight``.
+    (Where dx's sums cancel below 2^-6 of their terms, hand dy over in float32: binary32 sums for both.)
 
     ``w_columns`` and ``x_columns``: W (n x k) and x (rows x k) quantised along their columns, so
     k x n and k x rows.  ``need_dx=False`` leaves dx out (None)."""
@@ -338,7 +341,7 @@ def fp8_linear_backward(dy: torch.Tensor, w_columns: Fp8Matrix, x_columns: Fp8Ma
     _run("pact_fp8_linear_backward", index, _MATRIX.pack(dy.data_ptr(), m, n, ld, kind, 0), w_columns._bytes,
          x_columns._bytes, dx_packed, dw_packed, _FLAG_ACCUMULATE if accumulate else 0, at, nbytes)
     if grad_weight is not None:
-        _changed(dw)
+        _changed((dw,))
     return dx, dw
 
 
@@ -395,7 +398,7 @@ def _distill(name: str, logits, top_logits, top_index, temperature, row_weight, 
     if rc != PACT_OK:
         raise PactError(rc, name)
     if given is not None:
-        _changed(given)
+        _changed((given,))
     return loss, lse, grad
 
 
@@ -422,7 +425,8 @@ def distill_grad(logits: torch.Tensor, top_logits: torch.Tensor, top_index: torc
 def distill_step(logits: torch.Tensor, top_logits: torch.Tensor, top_index: torch.Tensor, temperature: float = 1.0,
                  row_weight: Optional[torch.Tensor] = None,
                  grad: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
-    """``(loss, grad)`` of one training step, the logits read once.  ``grad`` may be ``logits``: the
-    gradient then takes their place."""
+    """``(loss, grad)`` of one training step, the logits read once where a row fits a workgroup's registers
+    (up to 32768 entries of bfloat16, 65536 of float32) and twice, mostly from the caches, where it is longer.
+    ``grad`` may be ``logits``: the gradient then takes their place."""
     loss, _, grad = _distill("pact_distill_step", logits, top_logits, top_index, temperature, row_weight, grad, None, False)
     return loss, grad
